@@ -218,10 +218,7 @@ ff_status ln_backward_dispatch(ff_ctx* ctx, const LnBwd& p, int* parts, cudaStre
   if (p.cols <= 2048) return ln_backward_launch(ctx, ln_backward_kernel<T, 256, 1, CK, A>, p, 256, 1, 0, parts, st);
   if (p.cols <= 4096) return ln_backward_launch(ctx, ln_backward_kernel<T, 512, 1, CK, A>, p, 512, 1, 0, parts, st);
   if (p.cols <= LN_MAX_COLS) return ln_backward_launch(ctx, ln_backward_kernel<T, 512, 2, CK, A>, p, 512, 1, 0, parts, st);
-  if (p.dx) {
-    ln_backward_long_kernel<T, CK, A><<<(unsigned)p.rows, LN_LONG_THREADS, 0, st>>>(p);
-    FF_LAUNCH_CHECK(ctx);
-  }
+  // the sums first: they read dY, which dX may overwrite
   if (p.part) {
     const int gx = (p.cols + 255) / 256;
     long long gy = (8LL * ctx->sm_count + gx - 1) / gx;
@@ -231,6 +228,10 @@ ff_status ln_backward_dispatch(ff_ctx* ctx, const LnBwd& p, int* parts, cudaStre
     gy = (p.rows + rows_per - 1) / rows_per;
     *parts = (int)gy;
     ln_column_sums_kernel<T, CK, A><<<dim3(gx, (unsigned)gy), 256, 0, st>>>(p, rows_per);
+    FF_LAUNCH_CHECK(ctx);
+  }
+  if (p.dx) {
+    ln_backward_long_kernel<T, CK, A><<<(unsigned)p.rows, LN_LONG_THREADS, 0, st>>>(p);
     FF_LAUNCH_CHECK(ctx);
   }
   return FF_OK;

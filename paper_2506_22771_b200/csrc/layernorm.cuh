@@ -646,10 +646,11 @@ __global__ void __launch_bounds__(TEAM > 256 ? TEAM : 256, TEAM <= 256 ? 2 : 1) 
   if (p.part) ln_leave_sums<TEAM, TEAMS, V>(p, dg, db, t, team, acc);
 }
 
-// Any row length: a CTA per row reads it twice; the sums over rows are ln_column_sums_kernel's.
+// Any row length: a CTA per row reads it twice; the sums over rows are ln_column_sums_kernel's, which runs before this one.
 template <typename T, bool CK, int A>
 __global__ void __launch_bounds__(LN_LONG_THREADS) ln_backward_long_kernel(const LnBwd p) {
   __shared__ float sm[2][32];
+  dependents_may_start();
   const long long row = blockIdx.x;
   const float mean = CK ? 0.0f : p.mean[row], rstd = p.rstd[row];
   const T* dy = static_cast<const T*>(p.dy) + row * p.ld_dy;

@@ -1,0 +1,52 @@
+"""GPU tests of the block operators where a call's parts meet: outputs written over inputs, workspaces smaller than the most that a
+call can use, infinities beside bias sums.  Tolerances are those of test_gpu_block_ops.py unless a test states its own."""
+import numpy as np
+import pytest
+
+from oracle import block_ops as O
+from paper_2506_22771_b200 import binding as ffb
+from tests.test_gpu_block_ops import TYPES, U, Pitched, Saved, _data, _vec
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    c = ffb.Context(workspace_bytes=64 << 20)
+    yield c.ctx
+    c.close()
+
+
+# ---- layer norm backward in place --------------------------------------------------------------------------------------
+@pytest.mark.parametrize("ckpt", [True, False])
+@pytest.mark.parametrize("into", ["dy", "add"])
+@pytest.mark.parametrize("cols", [64, 500, 2000, 8192, 9000, 20011])
+def test_layernorm_parameter_sums_in_place(ctx, cols, into, ckpt):
+    """dX over dY or over dAdd leaves all three outputs with the bits of the call that writes elsewhere, and the sums right."""
+    import torch
+    rows = 37
+    g, x = _data(rows, cols, cols + 1)
+    dy, add = g.normal(size=(rows, cols)), g.normal(size=(rows, cols))
+    _, m, r, xh = O.layernorm_forward(Pitched(rows, cols, "bf16", values=x).np(), None, None, 1e-5)
+    X, c, mean, rstd = Pitched(rows, cols, "bf16", values=x), Saved(rows, cols, xh), _vec(m), _vec(r)
+
+    def run(into):
+        D, A = Pitched(rows, cols, "bf16", values=dy), Pitched(rows, cols, "bf16", values=add)
+        to = {"dy": D, "add": A, None: Pitched(rows, cols, "bf16")}[into]
+        dg, db = torch.zeros(cols, device="cuda"), torch.zeros(cols, device="cuda")
+        b = ffb.ff_layernorm_bufs(dY=D.ptr, ld_dy=D.ld, dAdd=A.ptr, ld_dadd=A.ld, rstd=rstd.data_ptr(), dX=to.ptr, ld_dx=to.ld,
+                                  dgamma=dg.data_ptr(), dbeta=db.data_ptr())
+        if ckpt:
+            b.C = c.struct
+        else:
+            b.X, b.ld_x, b.mean = X.ptr, X.ld, mean.data_ptr()
+        ffb.ff_layernorm_backward(ctx, ffb.ff_layernorm_desc(cols=cols, dtype=ffb.FF_BF16), b, rows)
+        return to.np(), dg.double().cpu().numpy(), db.double().cpu().numpy(), D
+
+    whole, there = run(None), run(into)
+    for k in range(3):
+        assert np.array_equal(whole[k], there[k])
+    d = whole[3].np()
+    assert (np.abs(there[2] - d.sum(axis=0)) <= 96 * U * np.abs(d).sum(axis=0)).all()
+    if ckpt:
+        assert (np.abs(there[1] - (d * c.values).sum(axis=0)) <= 96 * U * np.abs(d * c.values).sum(axis=0)).all()
