@@ -366,6 +366,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(WG_THREADS, 1)
       if (whole && p.db_part && n_warp + lane < N) {
         for (int i = 0; i < p.db_parts; ++i) db += p.db_part[(size_t)i * N + n_warp + lane];
         if (p.db && c.k0 == 0 && side == 0) p.db[n_warp + lane] = p.accumulate ? p.db[n_warp + lane] + db : db;
+        if (!beta) db = 0.0f;   // an infinite sum times no beta would be NaN
       }
       float acc[4][32];
 #pragma unroll

@@ -50,3 +50,35 @@ def test_layernorm_parameter_sums_in_place(ctx, cols, into, ckpt):
     assert (np.abs(there[2] - d.sum(axis=0)) <= 96 * U * np.abs(d).sum(axis=0)).all()
     if ckpt:
         assert (np.abs(there[1] - (d * c.values).sum(axis=0)) <= 96 * U * np.abs(d * c.values).sum(axis=0)).all()
+
+
+# ---- weight gradient: infinities ---------------------------------------------------------------------------------------
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("rows,n,cols,shift", [(70, 40, 96, 0), (70, 40, 95, 0), (70, 40, 96, 1), (5000, 17, 40, 0), (5000, 17, 39, 0)])
+def test_infinite_bias_sum_stays_in_the_bias(ctx, rows, n, cols, shift, kind):
+    """Without beta, dW does not depend on the sums of dY: an Inf there gives what the products alone give, whether the bias
+    gradient is asked for or not, in whole words or value by value, with one split or several."""
+    import torch
+    g = np.random.default_rng(cols + rows)
+    dy = g.normal(size=(rows, n))
+    dy[3, 5] = np.inf
+    D, c = Pitched(rows, n, kind, values=dy), Saved(rows, cols, g.normal(size=(rows, cols)) + 3.0)
+    ga = _vec(1 + 0.3 * g.normal(size=cols))
+    want, _ = O.wgrad(D.np(), c.values)
+    assert (np.abs(c.values[3]) > 0).all() and np.isinf(want[5]).all()
+    for gamma in (False, True):
+        out = []
+        for bias in (False, True):
+            dw, db = torch.full((n * cols + 4,), 7.0, device="cuda"), torch.zeros(n, device="cuda")
+            b = ffb.ff_ckpt8_wgrad_bufs(dY=D.ptr, ld_dy=D.ld, C=c.struct, dW=dw[shift:].data_ptr(), dbias=db.data_ptr() if bias else None)
+            if gamma:
+                b.gamma = ga.data_ptr()
+            ffb.ff_ckpt8_wgrad(ctx, ffb.ff_ckpt8_wgrad_desc(N=n, K=cols, dtype=TYPES[kind][0]), b, rows)
+            ffb.ff_poll_status(ctx)
+            out.append(dw[shift:shift + n * cols].double().cpu().numpy().reshape(n, cols))
+            if bias:
+                b = db.cpu().numpy()
+                assert b[5] == np.inf and np.isfinite(np.delete(b, 5)).all()
+        assert np.array_equal(out[0], out[1])
+        assert np.array_equal(np.isinf(out[1]), np.isinf(want)) and not np.isnan(out[1]).any()
+        assert np.array_equal(np.sign(out[1][5]), np.sign(want[5] * (ga.cpu().numpy() if gamma else 1.0)))
