@@ -501,7 +501,8 @@ ff_status ff_activation_backward(ff_ctx* ctx, const ff_activation_desc* desc, co
                                  void* cuda_stream);
 
 /* Weight and bias gradient of a linear layer y = x * W^T + b whose input is held as a checkpoint:
- *   dW[n,k] = sum_m dY[m,n] * X[m,k], dbias[n] = sum_m dY[m,n]   (FP32 sums of exact products)
+ *   dW[n,k] = sum_m dY[m,n] * X[m,k], dbias[n] = sum_m dY[m,n]   (FP32 sums of exact products;
+ * of FP32 dY the bits below 2^-133 are cut off)
  * With gamma / beta the checkpoint holds a layer norm's (x - mean) * rstd and the layer's input was its output:
  *   X[m,k] = C[m,k] * gamma[k] + beta[k]; one checkpoint serves the norm's backward pass and this. */
 typedef struct {

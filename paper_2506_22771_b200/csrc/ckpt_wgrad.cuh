@@ -6,11 +6,16 @@
 //
 // The contraction runs on tcgen05 kind::f16 with bfloat16 operands and FP32 accumulators.  A checkpoint's value has at
 // most 7 significant bits, so it is exact in bfloat16; dY is taken as a sum of bfloat16 parts that is exact: one part
-// for bfloat16, two for half (8 + 3 bits), three for FP32 (3 x 8 bits).  Every product is then exact.
+// for bfloat16, two for half (8 + 3 bits), three for FP32 (3 x 8 bits; of values below 2^-110 the bits under 2^-133, bfloat16's
+// smallest subnormal, are cut off).  Every product is then exact.
 //
 // The tensor core's accumulator truncates: summing S steps of 16 rows moves a sum of random terms by about
 // 2^-24 * 2/3 * S of itself (measured with a library product: 4.7e-7 at 512 rows, 1.9e-5 at 16384).  So the accumulator is
-// emptied every WG_CHUNK_STEPS steps and the chunks are added in FP32 registers, which rounds to nearest.
+// emptied every WG_CHUNK_STEPS steps (one stage, 12 steps, with three parts) and the chunks are added in FP32 registers, which
+// rounds to nearest.  A step truncates by the accumulator's size, however small its own products: a stage takes the lowest parts
+// of dY first, while the accumulator is small
+// (128 rows of FP32 dY, 500 x 784: 6.3e-8 of the result; chunks of 24 steps with the leading part first had 5.8e-7, a product in
+// FP32 has 2.0e-7; 8192 x 2000 x 2000 takes 167 us either way).
 //
 // Two kernels.  wgrad_prepare_kernel writes the checkpoint's values as bfloat16 into the workspace (and the parts of a dY
 // that is not bfloat16 with 16-byte rows), and sums dY's columns on the way.  wgrad_gemm_kernel is a matrix product fed by
@@ -61,7 +66,7 @@ struct WgGeom {
   static constexpr int STAGES = PARTS == 1 ? 6 : PARTS == 2 ? 4 : 3;
   static constexpr uint32_t SMEM_BYTES = STAGES * STAGE_BYTES + 8 * WG_PATCH_BYTES + 1024 + 512;
   static_assert(SMEM_BYTES <= 227 * 1024, "shared memory");
-  static constexpr int CHUNK_STAGES = WG_CHUNK_STEPS / (PARTS * (WG_ROWS / 16)) > 0 ? WG_CHUNK_STEPS / (PARTS * (WG_ROWS / 16)) : 1;
+  static constexpr int CHUNK_STAGES = PARTS == 3 ? 1 : WG_CHUNK_STEPS / (PARTS * (WG_ROWS / 16));
 };
 
 // D = FP32, A and B = bfloat16, both MN-major, M = 256 over the CTA pair
@@ -327,7 +332,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(WG_THREADS, 1)
               const uint32_t a0 = smem_desc_lo(ring + r.s * G::STAGE_BYTES, WG_ROWS * 128);
               const uint32_t b0 = a0 + ((PARTS * WG_TILE_BYTES) >> 4);
 #pragma unroll
-              for (int i = 0; i < PARTS; ++i) {
+              for (int i = PARTS - 1; i >= 0; --i) {
 #pragma unroll
                 for (int k = 0; k < WG_ROWS / 16; ++k) {
                   wg_mma(tmem_base + t.s * 256, smem_desc_join(a0 + i * (WG_TILE_BYTES >> 4) + k * 128, hi), smem_desc_join(b0 + k * 128, hi), idesc, acc);

@@ -82,3 +82,26 @@ def test_infinite_bias_sum_stays_in_the_bias(ctx, rows, n, cols, shift, kind):
         assert np.array_equal(out[0], out[1])
         assert np.array_equal(np.isinf(out[1]), np.isinf(want)) and not np.isnan(out[1]).any()
         assert np.array_equal(np.sign(out[1][5]), np.sign(want[5] * (ga.cpu().numpy() if gamma else 1.0)))
+
+
+# ---- weight gradient: accuracy of FP32 gradients -------------------------------------------------------------------------
+@pytest.mark.parametrize("rows,n,cols", [(64, 500, 784), (128, 500, 784), (512, 500, 784), (2048, 300, 520), (8192, 300, 520)])
+def test_weight_gradient_of_fp32_is_as_exact_as_fp32_products(rows, n, cols):
+    """The lower parts of dY enter a small accumulator, so what truncates is the four steps of the leading part in a stage: 2^-23 of
+    the accumulator each at most, half of that on average, 4 * 2^-24 = 2.4e-7 for a chunk.  Chunks are added with rounding to
+    nearest (2^-24 each, in both directions): 2^-24 * sqrt(chunks / 3) more, less than 4e-7 altogether at 8192 rows and 2.6e-7 at 128.
+    FP32 sums in order have 2^-24 * sqrt(rows / 3) and above."""
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(rows)
+    dy = torch.randn((rows, n), generator=gen, device="cuda") * 0.02
+    x = torch.randn((rows, cols), generator=gen, device="cuda")
+    d = ffb.ff_ckpt8_wgrad_desc(N=n, K=cols, dtype=ffb.FF_F32)
+    own = ffb.Context(workspace_bytes=ffb.ff_ckpt8_wgrad_workspace_bytes(d, rows))
+    c, dw = ffb.Ckpt8(rows, cols, "cuda"), torch.empty((n, cols), device="cuda")
+    ffb.ff_ckpt8_save(own.ctx, x.data_ptr(), cols, ffb.FF_F32, rows, cols, c.struct)
+    ffb.ff_ckpt8_wgrad(own.ctx, d, ffb.ff_ckpt8_wgrad_bufs(dY=dy.data_ptr(), ld_dy=n, C=c.struct, dW=dw.data_ptr()), rows)
+    ffb.ff_poll_status(own.ctx)
+    held = c.q.double() * torch.exp2(c.e.double() - 127).repeat_interleave(32, dim=1)[:, :cols]
+    want = dy.double().t() @ held
+    assert float((dw.double() - want).norm() / want.norm()) <= U * (4 + (rows / 64 / 3) ** 0.5)
+    own.close()
