@@ -117,6 +117,13 @@ struct LnRing {
   __device__ __forceinline__ void step() {
     if (++s == slots) s = 0, ph ^= 1u;
   }
+  // Before a thread ends: where a wait ran out, copies may still be on their way into the CTA's shared memory.
+  __device__ __forceinline__ void leave() const {
+    if (!dead) return;
+    const unsigned long long t0 = globaltimer_ns();
+    while (globaltimer_ns() - t0 < 2000000ull) {
+    }
+  }
 };
 __device__ __forceinline__ void copy_word(uint32_t dst, const void* src, int bytes) {   // four bytes, zeros past `bytes`
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
@@ -437,12 +444,14 @@ __global__ void __launch_bounds__((TEAM > 256 ? TEAM : 256) + 32, TEAM > 256 ? 1
     const int nb = (p.cols + C8_BLOCK - 1) / C8_BLOCK;
     LnRing empty;
     empty.slots = p.slots, empty.slot_bytes = 0, empty.base = 0, empty.ph = 1u;
-    for (long long base = (long long)blockIdx.x * (TEAMS * R); base < p.rows; base += step) {
+    bool going = true;   // no copies into a slot that was not given back: the teams' waits for them run out, too
+    for (long long base = (long long)blockIdx.x * (TEAMS * R); base < p.rows && going; base += step) {
       for (int q = 0; q < TEAMS; ++q) {
         const long long row0 = base + q * R;
         if (row0 >= p.rows) break;
         empty.bar = smem_u32(bars[1]) + q * LN_MAX_SLOTS * 8;
         empty.wait(p.status);
+        if (!(going = !__any_sync(0xffffffffu, empty.dead))) break;
         const uint32_t slot = ring0 + (q * p.slots + empty.s) * slot_bytes, bar = smem_u32(bars[0]) + (q * LN_MAX_SLOTS + empty.s) * 8;
         const int live = p.rows - row0 < R ? (int)(p.rows - row0) : R;
         if (lane == 0) mbar_expect_tx(bar, live * (dy_bytes + x_bytes + (p.dadd ? dy_bytes : 0u)));
@@ -467,6 +476,7 @@ __global__ void __launch_bounds__((TEAM > 256 ? TEAM : 256) + 32, TEAM > 256 ? 1
       }
       empty.step();
     }
+    empty.leave();
     return;
   }
 
@@ -555,6 +565,7 @@ __global__ void __launch_bounds__((TEAM > 256 ? TEAM : 256) + 32, TEAM > 256 ? 1
     if (lane == 0) mbar_arrive(done);
     ring.step();
   }
+  ring.leave();
   if (p.part) ln_leave_sums<TEAM, TEAMS, V>(p, dg, db, t, team, acc);
 }
 
