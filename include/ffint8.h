@@ -520,7 +520,9 @@ typedef struct {
   float* dbias;        /* [N], nullable                                                                      */
 } ff_ckpt8_wgrad_bufs;
 /* Workspace: the input in bfloat16 (2 bytes a value) and, for a dY that is not FF_BF16 with 16-byte rows, its parts (2 bytes
- * a value each: one part for FF_BF16, two for FF_F16, three for FF_F32), partial sums on top. */
+ * a value each: one part for FF_BF16, two for FF_F16, three for FF_F32), sums of dY's columns, partial sums on top.  What is
+ * asked for `rows` serves every smaller number of rows, and a device with any number of SMs: the contraction is cut into
+ * as many splits as the partial sums have room for. */
 ff_status ff_ckpt8_wgrad_workspace_bytes(const ff_ckpt8_wgrad_desc* desc, int64_t rows, size_t* out_bytes);
 ff_status ff_ckpt8_wgrad(ff_ctx* ctx, const ff_ckpt8_wgrad_desc* desc, const ff_ckpt8_wgrad_bufs* bufs, int64_t rows, void* cuda_stream);
 

@@ -477,8 +477,8 @@ ff_status ff_activation_backward(ff_ctx* ctx, const ff_activation_desc* d, const
 
 ff_status ff_ckpt8_wgrad_workspace_bytes(const ff_ckpt8_wgrad_desc* d, int64_t rows, size_t* out_bytes) {
   if (!d || !out_bytes || d->N <= 0 || d->K <= 0 || !known_dtype(d->dtype) || rows < 0 || rows > BLOCK_MAX_ROWS) return FF_ERR_ARG;
-  // the CTA pairs of a 148-SM device; a bfloat16 dY may turn out to need a copy with aligned rows
-  const WgPlan pl = wg_plan(rows, d->N, d->K, wgrad_parts(d->dtype), true, true, 74);
+  // the splits that the CTA pairs of a 148-SM device want; a bfloat16 dY may turn out to need a copy with aligned rows
+  const WgPlan pl = wg_plan(rows, d->N, d->K, wgrad_parts(d->dtype), true, true, 74, SIZE_MAX);
   *out_bytes = WS_BYTES + pl.x_bytes + pl.parts_bytes + pl.db_bytes + pl.part_bytes;
   return FF_OK;
 }
@@ -505,7 +505,8 @@ ff_status ff_ckpt8_wgrad(ff_ctx* ctx, const ff_ckpt8_wgrad_desc* d, const ff_ckp
   const unsigned al = row_alignment(b->dY, b->ld_dy, d->dtype);
   const bool split = !(d->dtype == FF_BF16 && al == 16);   // dY itself cannot be the operand
   const bool sums = rows && (b->dbias || b->beta);
-  const WgPlan pl = wg_plan(rows, d->N, d->K, wgrad_parts(d->dtype), split, sums, ctx->sm_count / 2);
+  const WgPlan pl = wg_plan(rows, d->N, d->K, wgrad_parts(d->dtype), split, sums, ctx->sm_count / 2,
+                            ctx->workspace_bytes - WS_BYTES);   // ff_set_workspace takes no less than WS_BYTES
   const size_t need = WS_BYTES + pl.x_bytes + pl.parts_bytes + pl.db_bytes + pl.part_bytes;
   if (ctx->workspace_bytes < need) return fail(ctx, FF_ERR_WORKSPACE, "workspace too small (ff_ckpt8_wgrad_workspace_bytes): needs %s%lld", "", (long long)need);
   if ((s = ensure_status(ctx, st)) != FF_OK) return s;

@@ -489,6 +489,8 @@ __global__ void __launch_bounds__(256) wgrad_join_kernel(const WgradArgs p, int 
 // How a weight gradient is cut.  Cost in clocks of an SM pair: an MMA of 16 rows takes max(bn / 2, 80) clocks (below 160
 // columns the operands' loads count), an item 4000 on top (pipeline fill, epilogue), and partial sums go through L2 once
 // each way.
+// Only the splits depend on the room that the workspace has left for their partial sums: the rest grows with the rows, and one split
+// needs none, so what is enough for a batch is enough for every smaller one, and for a device with another number of SMs.
 struct WgPlan {
   int bn, tiles_n, tiles_k, splits, stages_per_split, stages, db_parts, dy_lanes;
   long long db_rows, ld_x, ld_parts;
@@ -496,8 +498,24 @@ struct WgPlan {
 };
 constexpr int WG_DB_PARTS = 64;
 constexpr size_t WG_PART_CAP = (size_t)256 << 20;   // bytes of partial sums
-inline WgPlan wg_plan(long long rows, int N, int K, int parts, bool split_dy, bool sums, int groups) {
+inline WgPlan wg_plan(long long rows, int N, int K, int parts, bool split_dy, bool sums, int groups, size_t workspace_bytes) {
   WgPlan best{};
+  auto up = [](size_t v) { return (v + 255) / 256 * 256; };
+  // dY's share of a block of the preparation: lanes over its columns, and four rows of each of the others at least.  Sums over
+  // rows have at most 64 parts (narrow dY: 256), which the product's epilogue adds.
+  best.dy_lanes = 32;
+  while (best.dy_lanes > 1 && best.dy_lanes * 4 >= N) best.dy_lanes /= 2;
+  const long long least = 8 * (256 / best.dy_lanes), most = !sums ? rows : best.dy_lanes < 32 ? 4 * WG_DB_PARTS : WG_DB_PARTS;
+  long long gy = (rows + least - 1) / least;
+  if (gy > most) gy = most;
+  best.db_rows = gy ? (rows + gy - 1) / gy : 1;
+  best.db_parts = (int)((rows + best.db_rows - 1) / best.db_rows);
+  best.ld_x = ((long long)K + 15) / 16 * 16, best.ld_parts = ((long long)N + 7) / 8 * 8;
+  best.x_bytes = up((size_t)rows * best.ld_x * 2);
+  best.parts_bytes = split_dy ? up((size_t)parts * rows * best.ld_parts * 2) : 0;
+  best.db_bytes = sums ? up((size_t)gy * N * sizeof(float)) : 0;
+  const size_t fixed = best.x_bytes + best.parts_bytes + best.db_bytes, left = workspace_bytes > fixed ? workspace_bytes - fixed : 0;
+  const size_t room = left < WG_PART_CAP ? left : WG_PART_CAP;
   const int stages = (int)((rows + WG_ROWS - 1) / WG_ROWS);
   const int tiles_n = (N + 255) / 256;
   double best_cost = 0.0;
@@ -510,7 +528,7 @@ inline WgPlan wg_plan(long long rows, int N, int K, int parts, bool split_dy, bo
     for (int want = 1; want <= 64 && want <= stages; ++want) {
       const int per = (stages + want - 1) / want, splits = (stages + per - 1) / per;
       if (splits != want) continue;
-      if (splits > 1 && (size_t)splits * N * K * sizeof(float) > WG_PART_CAP) break;
+      if (splits > 1 && up((size_t)splits * N * K * sizeof(float)) > room) break;
       const long long items = tiles * splits, waves = (items + groups - 1) / groups;
       double cost = (double)waves * (per * stage_clk + 4000.0);
       if (splits > 1) cost += 6000.0 + (double)splits * N * K * 8.0 / 2000.0;
@@ -520,20 +538,6 @@ inline WgPlan wg_plan(long long rows, int N, int K, int parts, bool split_dy, bo
       }
     }
   }
-  // dY's share of a block of the preparation: lanes over its columns, and four rows of each of the others at least.  Sums over
-  // rows have at most 64 parts (narrow dY: 256), which the product's epilogue adds.
-  best.dy_lanes = 32;
-  while (best.dy_lanes > 1 && best.dy_lanes * 4 >= N) best.dy_lanes /= 2;
-  const long long least = 8 * (256 / best.dy_lanes), most = !sums ? rows : best.dy_lanes < 32 ? 4 * WG_DB_PARTS : WG_DB_PARTS;
-  long long gy = (rows + least - 1) / least;
-  if (gy > most) gy = most;
-  best.db_rows = gy ? (rows + gy - 1) / gy : 1;
-  best.db_parts = (int)((rows + best.db_rows - 1) / best.db_rows);
-  auto up = [](size_t v) { return (v + 255) / 256 * 256; };
-  best.ld_x = ((long long)K + 15) / 16 * 16, best.ld_parts = ((long long)N + 7) / 8 * 8;
-  best.x_bytes = up((size_t)rows * best.ld_x * 2);
-  best.parts_bytes = split_dy ? up((size_t)parts * rows * best.ld_parts * 2) : 0;
-  best.db_bytes = sums ? up((size_t)best.db_parts * N * sizeof(float)) : 0;
   best.part_bytes = best.splits > 1 ? up((size_t)best.splits * N * K * sizeof(float)) : 0;
   return best;
 }

@@ -84,6 +84,52 @@ def test_infinite_bias_sum_stays_in_the_bias(ctx, rows, n, cols, shift, kind):
         assert np.array_equal(np.sign(out[1][5]), np.sign(want[5] * (ga.cpu().numpy() if gamma else 1.0)))
 
 
+# ---- weight gradient: workspaces ---------------------------------------------------------------------------------------
+def _wgrad_in(workspace_bytes, rows, n, cols, kind):
+    import torch
+    g = np.random.default_rng(rows)
+    own = ffb.Context(workspace_bytes=workspace_bytes)
+    try:
+        D, c = Pitched(rows, n, kind, values=g.normal(size=(rows, n))), Saved(rows, cols, g.normal(size=(rows, cols)))
+        dw, db = torch.zeros((n, cols), device="cuda"), torch.zeros(n, device="cuda")
+        assert own.workspace.numel() == workspace_bytes
+        ffb.ff_ckpt8_wgrad(own.ctx, ffb.ff_ckpt8_wgrad_desc(N=n, K=cols, dtype=TYPES[kind][0]),
+                           ffb.ff_ckpt8_wgrad_bufs(dY=D.ptr, ld_dy=D.ld, C=c.struct, dW=dw.data_ptr(), dbias=db.data_ptr()), rows)
+        ffb.ff_poll_status(own.ctx)
+        wd, wb = O.wgrad(D.np(), c.values)
+        assert (np.abs(dw.double().cpu().numpy() - wd) <= 256 * U * (np.abs(D.np()).T @ np.abs(c.values))).all()
+        assert (np.abs(db.double().cpu().numpy() - wb) <= 256 * U * np.abs(D.np()).sum(axis=0)).all()
+    finally:
+        own.close()
+
+
+@pytest.mark.parametrize("kind,n,cols,most,rows", [("f32", 500, 784, 1281, 1280), ("f16", 500, 784, 1793, 1792), ("bf16", 300, 200, 2049, 2048),
+                                                   ("f32", 40, 24, 4097, 4095)])
+def test_workspace_of_the_largest_batch_serves_smaller_ones(kind, n, cols, most, rows):
+    """A program allocates for its batch; the last batch of a pass has fewer rows."""
+    d = ffb.ff_ckpt8_wgrad_desc(N=n, K=cols, dtype=TYPES[kind][0])
+    for r in (most, rows, 1):
+        _wgrad_in(ffb.ff_ckpt8_wgrad_workspace_bytes(d, most), r, n, cols, kind)
+
+
+@pytest.mark.parametrize("kind,parts", [("f32", 3), ("f16", 2), ("bf16", 1)])
+def test_workspace_without_room_for_splits_still_serves(kind, parts):
+    """The input, dY's parts and its column sums have to fit; the splits take what is left, none if nothing is (a device with
+    another number of SMs cuts the rows otherwise)."""
+    rows, n, cols = 3000, 300, 200
+    up = lambda v: -(-v // 256) * 256
+    d = ffb.ff_ckpt8_wgrad_desc(N=n, K=cols, dtype=TYPES[kind][0])
+    header = ffb.ff_ckpt8_wgrad_workspace_bytes(ffb.ff_ckpt8_wgrad_desc(N=1, K=1, dtype=ffb.FF_BF16), 0)
+    least = header + up(rows * 208 * 2) + up(parts * rows * 304 * 2) + up(-(-rows // 64) * n * 4)
+    asked = ffb.ff_ckpt8_wgrad_workspace_bytes(d, rows)
+    assert asked >= least + 2 * n * cols * 4, "the case is one that splits"
+    for room in (0, 1, 2 * n * cols * 4 + 256, 3 * n * cols * 4 + 256):
+        _wgrad_in(least + room, rows, n, cols, kind)
+    with pytest.raises(ffb.FFError) as e:
+        _wgrad_in(header + up(rows * 208 * 2), rows, n, cols, "f32")
+    assert e.value.code == ffb.FF_ERR_WORKSPACE
+
+
 # ---- weight gradient: accuracy of FP32 gradients -------------------------------------------------------------------------
 @pytest.mark.parametrize("rows,n,cols", [(64, 500, 784), (128, 500, 784), (512, 500, 784), (2048, 300, 520), (8192, 300, 520)])
 def test_weight_gradient_of_fp32_is_as_exact_as_fp32_products(rows, n, cols):
