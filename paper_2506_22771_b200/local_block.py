@@ -23,6 +23,20 @@ from . import binding as ffb
 _ACT = {"relu": ffb.FF_ACT_RELU, "gelu": ffb.FF_ACT_GELU, "silu": ffb.FF_ACT_SILU}
 
 
+def _address(name, t, rows, cols, dtype, device):
+    """(address, row pitch) of a tensor that the kernels are about to read; they see nothing but these, so its size, type, place and
+    strides have to be right."""
+    if tuple(t.shape) != (rows, cols):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, the block takes {(rows, cols)}")
+    if t.dtype != dtype:
+        raise ValueError(f"{name} is {t.dtype}, the block computes in {dtype}")
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, the block on {device}")
+    if (cols > 1 and t.stride(1) != 1) or (rows > 1 and t.stride(0) < cols):
+        raise ValueError(f"{name} has strides {t.stride()}; its rows have to be contiguous and apart from each other")
+    return t.data_ptr(), max(t.stride(0), cols)
+
+
 class LocalBlock:
     """Parameters, buffers and gradients of one block for batches of `rows` samples (positive and negative ones together)."""
 
@@ -31,7 +45,10 @@ class LocalBlock:
         import torch
         self.rows, self.width, self.hidden = rows, width, hidden
         self.dtype = dtype or torch.bfloat16
-        code = {torch.float32: ffb.FF_F32, torch.bfloat16: ffb.FF_BF16, torch.float16: ffb.FF_F16}[self.dtype]
+        codes = {torch.float32: ffb.FF_F32, torch.bfloat16: ffb.FF_BF16, torch.float16: ffb.FF_F16}
+        if act not in _ACT or self.dtype not in codes:
+            raise ValueError(f"act has to be one of {sorted(_ACT)}, dtype float32, bfloat16 or float16: {act!r}, {self.dtype}")
+        code = codes[self.dtype]
         dev = self.device = torch.device(f"cuda:{device_index}")
         gen = torch.Generator(device=dev).manual_seed(seed)
         new = lambda *s, t=torch.float32: torch.zeros(s, dtype=t, device=dev)
@@ -62,9 +79,11 @@ class LocalBlock:
     def forward(self, x, step: int):
         """y for x [rows, width]; fills the checkpoints."""
         import torch
+        x = x.detach()                                                # the gradient is `backward`'s, not autograd's
+        px, ld_x = _address("x", x, self.rows, self.width, self.dtype, self.device)
         st = torch.cuda.current_stream(self.device).cuda_stream
         ffb.ff_layernorm_forward(self.ctx.ctx, self.ln, ffb.ff_layernorm_bufs(
-            X=x.data_ptr(), ld_x=x.stride(0), gamma=self.gamma.data_ptr(), beta=self.beta.data_ptr(), Y=self.n.data_ptr(), ld_y=self.width,
+            X=px, ld_x=ld_x, gamma=self.gamma.data_ptr(), beta=self.beta.data_ptr(), Y=self.n.data_ptr(), ld_y=self.width,
             mean=self.mean.data_ptr(), rstd=self.rstd.data_ptr(), C=self.c_norm.struct), self.rows, step, st)
         h = self.n @ self.W1.to(self.dtype).t()
         ffb.ff_activation_forward(self.ctx.ctx, self.act, ffb.ff_activation_bufs(
@@ -74,9 +93,11 @@ class LocalBlock:
     def backward(self, dy):
         """dx for dy [rows, width]; leaves the parameters' gradients in dgamma, dbeta, dW1, dW2."""
         import torch
+        dy = dy.detach()
+        pdy, ld_dy = _address("dy", dy, self.rows, self.width, self.dtype, self.device)
         st = torch.cuda.current_stream(self.device).cuda_stream
         ctx = self.ctx.ctx
-        ffb.ff_ckpt8_wgrad(ctx, self.g2, ffb.ff_ckpt8_wgrad_bufs(dY=dy.data_ptr(), ld_dy=dy.stride(0), C=self.c_out.struct, dW=self.dW2.data_ptr()),
+        ffb.ff_ckpt8_wgrad(ctx, self.g2, ffb.ff_ckpt8_wgrad_bufs(dY=pdy, ld_dy=ld_dy, C=self.c_out.struct, dW=self.dW2.data_ptr()),
                            self.rows, st)
         dh = dy @ self.W2.to(self.dtype)
         ffb.ff_activation_backward(ctx, self.act, ffb.ff_activation_bufs(dZ=dh.data_ptr(), ld_dz=self.hidden, dH=dh.data_ptr(), ld_dh=self.hidden,
@@ -85,7 +106,7 @@ class LocalBlock:
                                                                  beta=self.beta.data_ptr(), dW=self.dW1.data_ptr()), self.rows, st)
         dx = dh @ self.W1.to(self.dtype)
         ffb.ff_layernorm_backward(ctx, self.ln, ffb.ff_layernorm_bufs(
-            dY=dx.data_ptr(), ld_dy=self.width, dAdd=dy.data_ptr(), ld_dadd=dy.stride(0), dX=dx.data_ptr(), ld_dx=self.width,
+            dY=dx.data_ptr(), ld_dy=self.width, dAdd=pdy, ld_dadd=ld_dy, dX=dx.data_ptr(), ld_dx=self.width,
             gamma=self.gamma.data_ptr(), rstd=self.rstd.data_ptr(), C=self.c_norm.struct, dgamma=self.dgamma.data_ptr(),
             dbeta=self.dbeta.data_ptr()), self.rows, st)
         return dx
