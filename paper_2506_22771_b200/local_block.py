@@ -6,9 +6,11 @@ pre-norm MLP in the place of such a layer,
     y = x + W2 act(W1 layernorm(x)),      goodness G = ||y||^2 per sample, losses of Eq. 1 / Eq. 2 against theta,
 
 so that the loss stays local to the block and the gradient is propagated inside it only.  Everything the block keeps between
-its forward and its backward pass is held in 8 bits: one checkpoint of the normalised input (it serves the layer norm's
-backward pass and, with gamma and beta folded in, the gradient of W1), one of the activation's input and one of its output.
-The two forward products and the two input gradients are plain matrix products.
+its forward and its backward pass is held in 8 bits (beside one FP32 number a row): one checkpoint of the normalised input (it
+serves the layer norm's backward pass and, with gamma and beta folded in, the gradient of W1), one of the activation's input
+and one of its output.  What a pass computes on the way is freed when it returns.  The workspace of the library's calls
+(2 bytes per value of the wider weight gradient's input and more) belongs to the context; blocks that run one after another
+on a stream share one.  The two forward products and the two input gradients are plain matrix products.
 
 Run as a program it trains a small block on seeded synthetic samples and prints the loss:
 
@@ -21,6 +23,17 @@ import argparse
 from . import binding as ffb
 
 _ACT = {"relu": ffb.FF_ACT_RELU, "gelu": ffb.FF_ACT_GELU, "silu": ffb.FF_ACT_SILU}
+
+
+def _descs(width, hidden, dtype):
+    """Descriptors whose workspaces a block needs: the layer norm's and the two weight gradients'."""
+    import torch
+    codes = {torch.float32: ffb.FF_F32, torch.bfloat16: ffb.FF_BF16, torch.float16: ffb.FF_F16}
+    if dtype not in codes:
+        raise ValueError(f"dtype has to be float32, bfloat16 or float16: {dtype}")
+    code = codes[dtype]
+    return (ffb.ff_layernorm_desc(cols=width, dtype=code, index=0), ffb.ff_ckpt8_wgrad_desc(N=hidden, K=width, dtype=code),
+            ffb.ff_ckpt8_wgrad_desc(N=width, K=hidden, dtype=code))
 
 
 def _address(name, t, rows, cols, dtype, device):
@@ -38,42 +51,50 @@ def _address(name, t, rows, cols, dtype, device):
 
 
 class LocalBlock:
-    """Parameters, buffers and gradients of one block for batches of `rows` samples (positive and negative ones together)."""
+    """Parameters, checkpoints and gradients of one block for batches of `rows` samples (positive and negative ones together).
+    context: a binding.Context that blocks share, with at least the `workspace_bytes` of each; by default the block has its own."""
 
     def __init__(self, rows: int, width: int, hidden: int, act: str = "gelu", dtype=None, eps: float = 1e-5, seed: int = 0,
-                 stochastic: bool = True, device_index: int = 0):
+                 stochastic: bool = True, device_index: int = 0, context=None):
         import torch
         self.rows, self.width, self.hidden = rows, width, hidden
         self.dtype = dtype or torch.bfloat16
-        codes = {torch.float32: ffb.FF_F32, torch.bfloat16: ffb.FF_BF16, torch.float16: ffb.FF_F16}
-        if act not in _ACT or self.dtype not in codes:
-            raise ValueError(f"act has to be one of {sorted(_ACT)}, dtype float32, bfloat16 or float16: {act!r}, {self.dtype}")
-        code = codes[self.dtype]
+        if act not in _ACT:
+            raise ValueError(f"act has to be one of {sorted(_ACT)}: {act!r}")
+        self.ln, self.g1, self.g2 = _descs(width, hidden, self.dtype)
+        need = self.workspace_bytes(rows, width, hidden, self.dtype)
+        if context is not None and context.workspace.numel() < need:
+            raise ValueError(f"the context's workspace has {context.workspace.numel()} bytes, the block needs {need}")
         dev = self.device = torch.device(f"cuda:{device_index}")
         gen = torch.Generator(device=dev).manual_seed(seed)
-        new = lambda *s, t=torch.float32: torch.zeros(s, dtype=t, device=dev)
+        new = lambda *s: torch.zeros(s, device=dev)
         self.gamma, self.beta = torch.ones(width, device=dev), new(width)
         self.W1 = torch.randn((hidden, width), generator=gen, device=dev) * width ** -0.5
         self.W2 = torch.randn((width, hidden), generator=gen, device=dev) * (0.5 * hidden ** -0.5)
         self.dgamma, self.dbeta, self.dW1, self.dW2 = new(width), new(width), new(hidden, width), new(width, hidden)
-        self.n, self.z = new(rows, width, t=self.dtype), new(rows, hidden, t=self.dtype)
-        self.mean, self.rstd = new(rows), new(rows)
+        self.rstd = new(rows)
         self.c_norm, self.c_in, self.c_out = ffb.Ckpt8(rows, width, dev), ffb.Ckpt8(rows, hidden, dev), ffb.Ckpt8(rows, hidden, dev)
         rounding = ffb.FF_ROUND_STOCHASTIC if stochastic else ffb.FF_ROUND_NEAREST_EVEN
-        self.ln = ffb.ff_layernorm_desc(cols=width, dtype=code, eps=eps, round=rounding, seed=seed, index=0)
+        self.ln.eps, self.ln.round, self.ln.seed = eps, rounding, seed
         keep = ffb.FF_ROUND_KEEP_SIGN if act == "relu" else 0          # the slope of a ReLU is its input's sign
-        self.act = ffb.ff_activation_desc(kind=_ACT[act], cols=hidden, dtype=code, round=rounding | keep, seed=seed, index=1)
-        self.g1 = ffb.ff_ckpt8_wgrad_desc(N=hidden, K=width, dtype=code)
-        self.g2 = ffb.ff_ckpt8_wgrad_desc(N=width, K=hidden, dtype=code)
-        self.ctx = ffb.Context(device_index=device_index, workspace_bytes=max(
-            ffb.ff_layernorm_workspace_bytes(self.ln, rows), ffb.ff_ckpt8_wgrad_workspace_bytes(self.g1, rows),
-            ffb.ff_ckpt8_wgrad_workspace_bytes(self.g2, rows)))
+        self.act = ffb.ff_activation_desc(kind=_ACT[act], cols=hidden, dtype=self.ln.dtype, round=rounding | keep, seed=seed, index=1)
+        self._own = context is None
+        self.ctx = ffb.Context(device_index=device_index, workspace_bytes=need) if self._own else context
+
+    @staticmethod
+    def workspace_bytes(rows: int, width: int, hidden: int, dtype=None) -> int:
+        """Workspace of a context that a block of these sizes (or smaller batches of it) runs on."""
+        import torch
+        ln, g1, g2 = _descs(width, hidden, dtype or torch.bfloat16)
+        return max(ffb.ff_layernorm_workspace_bytes(ln, rows), ffb.ff_ckpt8_wgrad_workspace_bytes(g1, rows),
+                   ffb.ff_ckpt8_wgrad_workspace_bytes(g2, rows))
 
     def close(self):
-        self.ctx.close()
+        if self._own:
+            self.ctx.close()
 
     def saved_bytes(self) -> int:
-        """What stays alive from the forward to the backward pass, per-row statistics included."""
+        """What the block holds from the forward to the backward pass: its checkpoints and one FP32 number a row."""
         return sum(c._q.numel() + c.e.numel() for c in (self.c_norm, self.c_in, self.c_out)) + 4 * self.rows
 
     def forward(self, x, step: int):
@@ -81,14 +102,15 @@ class LocalBlock:
         import torch
         x = x.detach()                                                # the gradient is `backward`'s, not autograd's
         px, ld_x = _address("x", x, self.rows, self.width, self.dtype, self.device)
+        n = torch.empty((self.rows, self.width), dtype=self.dtype, device=self.device)
         st = torch.cuda.current_stream(self.device).cuda_stream
         ffb.ff_layernorm_forward(self.ctx.ctx, self.ln, ffb.ff_layernorm_bufs(
-            X=px, ld_x=ld_x, gamma=self.gamma.data_ptr(), beta=self.beta.data_ptr(), Y=self.n.data_ptr(), ld_y=self.width,
-            mean=self.mean.data_ptr(), rstd=self.rstd.data_ptr(), C=self.c_norm.struct), self.rows, step, st)
-        h = self.n @ self.W1.to(self.dtype).t()
+            X=px, ld_x=ld_x, gamma=self.gamma.data_ptr(), beta=self.beta.data_ptr(), Y=n.data_ptr(), ld_y=self.width,
+            rstd=self.rstd.data_ptr(), C=self.c_norm.struct), self.rows, step, st)
+        h = n @ self.W1.to(self.dtype).t()
         ffb.ff_activation_forward(self.ctx.ctx, self.act, ffb.ff_activation_bufs(
-            H=h.data_ptr(), ld_h=self.hidden, Z=self.z.data_ptr(), ld_z=self.hidden, CH=self.c_in.struct, CZ=self.c_out.struct), self.rows, step, st)
-        return x + self.z @ self.W2.to(self.dtype).t()
+            H=h.data_ptr(), ld_h=self.hidden, Z=h.data_ptr(), ld_z=self.hidden, CH=self.c_in.struct, CZ=self.c_out.struct), self.rows, step, st)
+        return x + h @ self.W2.to(self.dtype).t()
 
     def backward(self, dy):
         """dx for dy [rows, width]; leaves the parameters' gradients in dgamma, dbeta, dW1, dW2."""
@@ -158,7 +180,8 @@ def main(argv=None):
     ffb.ff_poll_status(block.ctx.ctx)
     held = block.saved_bytes()
     plain = 2 * a.rows * (a.width + 2 * a.hidden)
-    print(f"held between the passes: {held} bytes ({held / plain:.2f} of 16-bit activations)")
+    print(f"held between the passes: {held} bytes ({held / plain:.2f} of 16-bit activations); "
+          f"workspace, which blocks can share: {block.ctx.workspace.numel()} bytes")
     block.close()
     return first, last
 
