@@ -102,7 +102,9 @@ inline int group_blocks(const GroupList& g) { return (int)((g.total + C8_THREADS
 
 // ---- layer norm -----------------------------------------------------------------------------
 constexpr int LN_MAX_COLS = 8192;       // longest row that a team keeps in registers
-constexpr int LN_MAX_PARTS = 592;       // most CTAs of a backward pass that sums over rows
+// Most CTAs of a backward pass that sums over rows, four an SM of 148.  What it limits is the workspace, not the kernels: one or two CTAs an
+// SM are resident (8192 x 2000 bfloat16 with at most 148 parts 37.9 us, with 296 to 1184 30.5; 60000 x 500 half 102 and 68).
+constexpr int LN_MAX_PARTS = 592;
 inline size_t ln_part_bytes(int cols, int64_t rows) {   // a CTA takes at least one row
   return (size_t)(rows < LN_MAX_PARTS ? rows : LN_MAX_PARTS) * 2 * cols * sizeof(float);
 }
@@ -153,7 +155,11 @@ ff_status ln_forward_dispatch(ff_ctx* ctx, const LnFwd& p, cudaStream_t st) {
   if (p.cols <= 64) return ln_forward_launch<T, 8, 1, 1, A>(ctx, p, st);
   if (p.cols <= 128) return ln_forward_launch<T, 16, 1, 1, A>(ctx, p, st);
   if (p.cols <= 256) return ln_forward_launch<T, 32, 1, 1, A>(ctx, p, st);
-  if (p.rows <= 4 * ctx->sm_count) {   // few rows: a group a thread, for the shortest way through a row
+  // Few rows: a group a thread, for the shortest way through a row, as long as the threads that fit the device (1024 an SM) hold
+  // the tensor, or nearly.  Against two groups a thread and two rows a team, bfloat16: 148 x 784 2.7 us against 4.4, 1184 x 784 3.7 against
+  // 4.5, 2368 x 784 5.9 against 5.1; 592 x 2000 3.7 against 4.5, 1184 x 2000 5.7 against 5.2; 148 x 8192 3.6 against 4.8, 296 x 8192
+  // 6.0 against 5.0, 592 x 8192 10.8 against 6.9.
+  if (3 * p.rows * p.cols <= 4LL * (1024 * C8_GROUP) * ctx->sm_count) {
     if (p.cols <= 512) return ln_forward_launch<T, 64, 1, 1, A>(ctx, p, st);
     if (p.cols <= 1024) return ln_forward_launch<T, 128, 1, 1, A>(ctx, p, st);
     if (p.cols <= 2048) return ln_forward_launch<T, 256, 1, 1, A>(ctx, p, st);
@@ -194,7 +200,8 @@ ff_status ln_backward_ring(ff_ctx* ctx, const LnBwd& p, int* parts, cudaStream_t
   // shared memory of one or two CTAs an SM, less what the kernel has for itself
   const size_t share = (size_t)(TEAM > 256 ? 220 : 110) * 1024 - 2048 - params - (teams > 1 ? ln_acc_floats<TEAM, teams, V>() * sizeof(float) : 0);
   LnBwd q = p;
-  // two rows a step where three steps fit the ring: half as many barriers (with two groups a thread there are no registers for it)
+  // two rows a step where three steps fit the ring: half as many barriers (with two groups a thread there are no registers for it).
+  // From the checkpoint, two rows against one: 32768 x 4096 bfloat16 160 us against 186, 16384 x 2048 FP32 58 against 65, 32768 x 1000 FP32 68 against 65.
   if constexpr (V == 1)
     if ((q.slots = ln_slots(teams * slot(2), share)) >= 3)
       return ln_backward_launch(ctx, ln_backward_ring_kernel<T, TEAM, V, 2, CK>, q, threads + 32, 2 * teams, params + q.slots * teams * slot(2), parts, st);
@@ -203,6 +210,8 @@ ff_status ln_backward_ring(ff_ctx* ctx, const LnBwd& p, int* parts, cudaStream_t
 }
 template <typename T, bool CK, int A>
 ff_status ln_backward_dispatch(ff_ctx* ctx, const LnBwd& p, int* parts, cudaStream_t st) {
+  // The ring against rows in registers, from the checkpoint, bfloat16: 65536 x 520 119 us against 119 (from x 97 against 121), 32768 x 1000 66 against
+  // 78, 65536 x 2000 163 against 296, 32768 x 8192 296 against 350; with one row a CTA (300 x 8192) 20 against 19.
   if constexpr (A == 16) {
     if (p.cols > 512 && p.cols <= LN_MAX_COLS && p.cols * sizeof(T) % 16 == 0 && (!CK || (reinterpret_cast<uintptr_t>(p.c.e) & 3) == 0)) {
       if (p.cols <= 1024) return ln_backward_ring<T, CK, 128, 1>(ctx, p, parts, st);

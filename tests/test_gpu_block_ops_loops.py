@@ -51,6 +51,43 @@ def _within(got, want, room, what):
     assert float(far.max()) <= 0.0, (what, float(far.max()), int((far > 0).sum()))
 
 
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("rows,cols,pad", [(9001, 64, 0), (9001, 200, 1), (6001, 300, 0), (3601, 500, 0), (2401, 784, 8), (2001, 1000, 3), (1101, 2000, 0),
+                                           (1001, 2001, 0), (601, 4096, 0), (501, 8192, 0), (301, 8191, 2)])
+def test_layernorm_forward_over_many_rows(ctx, gen, rows, cols, pad, kind):
+    """Two rows a team, the last one alone.  Without gamma and beta FP32's y is the normalised value, whose checkpoint is then the one that
+    ff_ckpt8_save makes of it, in every rounding mode."""
+    import torch
+    code, w, step = TYPES[kind]
+    X = _pitched(rows, cols, kind, pad, torch.randn((rows, cols), generator=gen, device="cuda") + 0.25)
+    gamma, beta = 1 + 0.3 * torch.randn(cols, generator=gen, device="cuda"), torch.randn(cols, generator=gen, device="cuda")
+    xd = X.double()
+    m = xd.mean(dim=1, keepdim=True)
+    r = ((xd - m).square().mean(dim=1, keepdim=True) + 1e-5).rsqrt()
+    xh, most = (xd - m) * r, xd.abs().amax(dim=1, keepdim=True)
+    dxh = 64 * U * (xh.abs() * (2 + r * most) + r * most)
+    for mode, affine in ((ffb.FF_ROUND_NEAREST_EVEN, True), (ffb.FF_ROUND_STOCHASTIC, False), (ffb.FF_ROUND_STOCHASTIC | ffb.FF_ROUND_KEEP_SIGN, False)):
+        Y, c = _pitched(rows, cols, kind, pad), ffb.Ckpt8(rows, cols, "cuda")
+        mean, rstd = torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+        b = ffb.ff_layernorm_bufs(X=X.data_ptr(), ld_x=X.stride(0), Y=Y.data_ptr(), ld_y=Y.stride(0), mean=mean.data_ptr(), rstd=rstd.data_ptr(), C=c.struct)
+        if affine:
+            b.gamma, b.beta = gamma.data_ptr(), beta.data_ptr()
+        d = ffb.ff_layernorm_desc(cols=cols, dtype=code, eps=1e-5, round=mode, seed=5, index=2)
+        ffb.ff_layernorm_forward(ctx, d, b, rows, 9)
+        ffb.ff_poll_status(ctx)
+        _within(mean, m[:, 0], 64 * U * most[:, 0], "mean")
+        _within(rstd, r[:, 0], (64 * U * r * (2 + r * most))[:, 0], "rstd")
+        y = xh * gamma.double() + beta.double() if affine else xh
+        dy = dxh * (gamma.double().abs() if affine else 1.0) + 2 * U * y.abs()
+        _within(Y, y, dy + w * (y.abs() + dy) + step, "y")
+        unit = torch.exp2(c.e.double() - 127).repeat_interleave(32, dim=1)[:, :cols]
+        _within(c.q.double() * unit, xh, (0.5 if mode == ffb.FF_ROUND_NEAREST_EVEN else 1.0) * unit * (1 + 2.0 ** -20) + dxh, "held")
+        if kind == "f32" and not affine:
+            own = ffb.Ckpt8(rows, cols, "cuda")
+            ffb.ff_ckpt8_save(ctx, Y.data_ptr(), Y.stride(0), ffb.FF_F32, rows, cols, own.struct, mode, 5, 2, 9)
+            assert torch.equal(own.q, c.q) and torch.equal(own.e, c.e)
+
+
 # rows of the ring kernel in each of its shapes, of the register kernels (narrow, and rows that bulk copies cannot address)
 @pytest.mark.parametrize("ckpt", [True, False])
 @pytest.mark.parametrize("kind,rows,cols,pad", [("bf16", 8192, 2000, 0), ("f32", 8192, 2000, 0), ("f16", 6000, 1000, 0), ("f32", 4000, 4096, 0),
