@@ -414,8 +414,9 @@ ff_status ff_loss_coef_static(const float* G, float theta, const float* const* G
  * keeps between its forward and its backward pass is held in 8 bits.
  *
  * Tensors are row-major [rows, cols] device arrays of one FF_F32 / FF_BF16 / FF_F16 type per call with a row pitch of
- * `ld_*` ELEMENTS (>= cols), aligned to their type; a base address and pitch that are multiples of 16 bytes and cols that
- * are a multiple of 8 take the vector path.  gamma, beta, statistics and parameter gradients are FP32.  rows = 0 is
+ * `ld_*` ELEMENTS (>= cols), aligned to their type.  Where base addresses and pitches are multiples of 16 (or 8) bytes, every
+ * whole group of 8 columns moves in words of that size, and only a group that the end of a row cuts goes value by value;
+ * rows aligned to their type alone go value by value throughout (1.4 to 7 times as long).  gamma, beta, statistics and parameter gradients are FP32.  rows = 0 is
  * allowed: sums over no rows are zeros.  Calls are asynchronous on the stream and allocate nothing; the workspace rules
  * of the context hold (calls that share it belong on one stream). */
 enum { FF_F32 = 0, FF_BF16 = 1, FF_F16 = 2 };

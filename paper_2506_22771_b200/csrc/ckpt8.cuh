@@ -9,8 +9,11 @@
 // A block whose maximum lies below 2^-100 is zero (the range rule of the library's INT8 quantiser).  A block with an
 // Inf or a NaN gets byte 255: its codes are zero, it restores to NaN (0 * Inf) and raises ST_NONFINITE.
 //
-// A thread owns a group of 8 consecutive columns, four neighbouring lanes a block.  All kernels here are bound by HBM
-// (5 to 8 bytes per value), so each thread issues the loads of several groups before it computes.
+// A thread owns a group of 8 consecutive columns, four neighbouring lanes a block, and issues the loads of several groups before
+// it computes.  Save, restore and the activations' backward pass are bound by HBM (3 to 9 bytes per value, 5.9 to 6.5 TB/s on rows
+// of whole 16-byte words), the activations' forward pass with two checkpoints by its instructions (8192 x 2000 bfloat16 28 us
+// against 15 of HBM), every form with stochastic rounding by the hash (save 9.5 us nearest, 21 stochastic; two checkpoints of GELU 28 and 52).
+// Rows aligned only to their type go value by value and are bound by these accesses (save 13 us, restore 53 against 7.4).
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -174,7 +177,7 @@ __device__ __forceinline__ uint32_t c8_encode(const float (&v)[8], uint32_t row,
   int q[8];
   if (!rd.stochastic) {
     // x * 2^-E is exact and at most 127, so adding 1.5 * 2^23 in the same operation leaves it rounded to nearest even
-    // in the low byte
+    // in the low byte (the sum's last place is 1)
 #pragma unroll
     for (int j = 0; j < 8; ++j) q[j] = (int)__float_as_uint(fmaf(v[j], inv, 12582912.0f));
   } else {
@@ -342,8 +345,9 @@ __device__ __forceinline__ float rcp_approx(float x) {
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
 }
-// Logistic function from e = e^-|h| <= 1 (no overflow).  The product with log2(e) carries a second term, so that large |h|
-// keep their digits; -1e30 stands for -Inf, whose terms would cancel to NaN (a NaN comes back through the callers' h).
+// Logistic function from e = e^-|h| <= 1 (no overflow).  e^x = 2^(x log2(e)): the product is kept in two terms, its own rounding error
+// and the part of log2(e) below FP32's last place (Dekker's product with a constant in two parts, as Cody and Waite reduce arguments), so
+// that large |h| keep their digits; the second term enters as 1 + its size.  -1e30 stands for -Inf, whose terms would cancel to NaN (a NaN comes back through the callers' h).
 __device__ __forceinline__ float logistic(float h) {
   const float x = fmaxf(-fabsf(h), -1e30f);
   const float t = x * 1.44269504f;
@@ -431,7 +435,7 @@ __global__ void __launch_bounds__(C8_THREADS) act_forward_kernel(const T* h, lon
 // dh = dz * act'(h), h from its checkpoint.  dh may be dz itself.
 // A code and an exponent decide the slope: the slopes of the 256 codes for exponents -13 .. 4 (blocks whose maximum lies
 // between 2^-7 and 2^11) stand in a table that each CTA computes with the same function, so a value costs a table read
-// instead of some 20 operations (317 us against 235 at 32768 x 8192 bfloat16, where HBM needs 206).  Other exponents are computed.
+// instead of some 20 operations (229 us against 318 at 32768 x 8192 bfloat16, where HBM needs 206).  Other exponents are computed.
 constexpr uint32_t ACT_E0 = 114, ACT_TABLES = 18;
 template <typename T, int KIND, int A>
 __global__ void __launch_bounds__(C8_THREADS) act_backward_kernel(const T* dz, long long ld_dz, C8View ch, T* dh, long long ld_dh, int cols,

@@ -15,13 +15,15 @@
 // rounds to nearest.  A step truncates by the accumulator's size, however small its own products: a stage takes the lowest parts
 // of dY first, while the accumulator is small
 // (128 rows of FP32 dY, 500 x 784: 6.3e-8 of the result; chunks of 24 steps with the leading part first had 5.8e-7, a product in
-// FP32 has 2.0e-7; 8192 x 2000 x 2000 takes 167 us either way).
+// FP32 has 2.0e-7; 8192 x 2000 x 2000 takes 167 us either way).  With one or two parts, chunks of 16 steps instead of 32 would
+// halve the error (bfloat16 512 x 500 x 784 1.0e-7 -> 6.0e-8, the FP32 product 5.7e-8) and cost 3 to 8 % (2048 x 2000 x 2000 29.6 -> 30.8 us,
+// half 8192 x 2000 x 784 92.9 -> 100); 32 stay, whose error no longer grows past 512 rows.
 //
 // Two kernels.  wgrad_prepare_kernel writes the checkpoint's values as bfloat16 into the workspace (and the parts of a dY
 // that is not bfloat16 with 16-byte rows), and sums dY's columns on the way.  wgrad_gemm_kernel is a matrix product fed by
 // TMA alone.  Expanding the codes inside the product was built first: its warps' chain of barrier waits, shared-memory
 // reads, expansion, fence and arrival took 800 to 900 clocks a stage of 64 rows against 512 of the MMAs, however the warps were
-// divided, and every tile row expanded the same codes again (4.4 ms against 2.9 at 32768 x 8192 x 8192).
+// divided, and every tile row expanded the same codes again (4.4 ms against 3.8 to 4.1 at 32768 x 8192 x 8192).
 //
 // A pair of CTAs (cta_group::2) owns a 256 (n) x bn (k) tile; each stages its 128 rows of n and its half of k.  Both
 // operands are read along their contiguous dimension, so both are MN-major: a stage holds 64 contraction rows as blocks
@@ -487,8 +489,10 @@ __global__ void __launch_bounds__(256) wgrad_join_kernel(const WgradArgs p, int 
 
 // ---- host side ----------------------------------------------------------------------------------
 // How a weight gradient is cut.  Cost in clocks of an SM pair: an MMA of 16 rows takes max(bn / 2, 80) clocks (below 160
-// columns the operands' loads count), an item 4000 on top (pipeline fill, epilogue), and partial sums go through L2 once
-// each way.
+// columns the operands' loads count), an item 4000 on top (pipeline fill, epilogue), a join 6000, and partial sums go through L2 once
+// each way (2000 bytes a clock).  The model was held against all tile widths and splits at ten shapes: its plan is the fastest or
+// within 8 % at eight; 8192 x 2000 x 784 half takes 86.7 us where two splits of 256 columns take 79.5, 16384 x 1000 x 1000 bfloat16
+// 66.6 where four take 55.9.  The slowest plans took 1.5 to 15 times as long.
 // Only the splits depend on the room that the workspace has left for their partial sums: the rest grows with the rows, and one split
 // needs none, so what is enough for a batch is enough for every smaller one, and for a device with another number of SMs.
 struct WgPlan {
@@ -496,6 +500,8 @@ struct WgPlan {
   long long db_rows, ld_x, ld_parts;
   size_t x_bytes, parts_bytes, db_bytes, part_bytes;   // of the workspace, multiples of 256
 };
+// Parts of dY's column sums: more make the preparation wider, fewer the epilogue's additions.  With 8, 32, 64, 128 parts: 8192 x 2000 x 784 half
+// 144, 97, 89, 88 us; 16384 x 4096 x 1024 bfloat16 157, 138, 146, 149; 2048 x 2000 x 2000 bfloat16 28.7, 25.2, 25.2, 25.3.
 constexpr int WG_DB_PARTS = 64;
 constexpr size_t WG_PART_CAP = (size_t)256 << 20;   // bytes of partial sums
 inline WgPlan wg_plan(long long rows, int N, int K, int parts, bool split_dy, bool sums, int groups, size_t workspace_bytes) {

@@ -5,7 +5,10 @@
 // All statistics and sums are FP32; the variance is taken from the centred values (a row stays in registers), so an
 // offset of the row costs no digits.  Sums over rows run in a fixed order (per CTA, then over CTAs): no atomics.
 //
-// Both directions are bound by HBM.  A team of TEAM threads owns a row, thread t the groups t, t + TEAM, ... of 8 columns.
+// HBM is the floor of both directions.  Forward with a checkpoint the instructions bound it (26 a value, 70 % of the issue slots:
+// 32768 x 8192 bfloat16 270 us against 206 of HBM); backward, with 27 a value and 59 % of the slots, latencies of arithmetic and shared
+// memory and the barrier of each step are not covered by the 16 computing warps of an SM (8192 x 2000 from the checkpoint with a residual
+// 33 us against 18).  A team of TEAM threads owns a row, thread t the groups t, t + TEAM, ... of 8 columns.
 // Forward, a team has one or two rows and many teams share an SM.  Backward, where a thread keeps sums for its columns over
 // many rows, teams walk over the rows: rows of more than 512 columns whose bytes are multiples of 16 arrive in shared memory
 // by bulk copies, a ring ahead of the team; others are loaded into registers one row ahead.
@@ -142,8 +145,9 @@ __device__ __forceinline__ Raw8<T> lds8(uint32_t src, int n) {
   return r;
 }
 
-// a / n from 1 / n with the remainder put right, and 1 / sqrt(a) with a Newton step: each within an ulp, in a few operations that
-// every thread of a row does.
+// a / n from 1 / n, corrected by its remainder a - q n, which one fused multiply-add gives exactly (the correction of a quotient that Markstein
+// described in 1990), and 1 / sqrt(a) with a step of Newton's method, r + r (1 - a r r) / 2: each within an ulp, in a few operations
+// that every thread of a row does.
 __device__ __forceinline__ float quotient(float a, float n, float inv_n) {
   const float q = a * inv_n;
   return fabsf(q) < __uint_as_float(0x7f800000u) ? fmaf(fmaf(-q, n, a), inv_n, q) : q;   // an infinite sum stays one
@@ -412,7 +416,7 @@ __device__ __forceinline__ void ln_leave_sums(const LnBwd& p, float (&dg)[V][8],
 
 // Rows through a ring of bulk copies: cols <= TEAM * 8 * V.  A step is R rows of a team, whose sums are reduced together; the
 // sums over the rows stay in registers, gamma is in shared memory.  One more warp asks for the rows, as far ahead as the
-// slots reach; done by the teams' own first warps, the others waited for them (219 us against 160 at 65536 x 2000).
+// slots reach; done by the teams' own first warps, the others waited for them (220 us against 168 at 65536 x 2000).
 template <typename T, int TEAM, int V, int R, bool CK>
 __global__ void __launch_bounds__((TEAM > 256 ? TEAM : 256) + 32, TEAM > 256 ? 1 : 2) ln_backward_ring_kernel(const LnBwd p) {
   constexpr int THREADS = TEAM > 256 ? TEAM : 256, TEAMS = THREADS / TEAM;
